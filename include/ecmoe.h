@@ -119,7 +119,8 @@ int64_t ec_rows_per_expert(const ec_ctx* ctx);
 size_t ec_workspace_bytes(const ec_ctx* ctx);
 
 /* Attach a caller-owned device workspace of at least ec_workspace_bytes bytes, 256-byte
- * aligned. Uploads the group table with a synchronous copy; call outside stream capture.
+ * aligned. Uploads the group table with a synchronous copy; call outside stream capture. Where that
+ * fails (EC_ERR_CUDA) no workspace is attached.
  * The workspace must stay allocated while the context is used. */
 ec_status ec_ctx_set_workspace(ec_ctx* ctx, void* workspace, size_t bytes);
 

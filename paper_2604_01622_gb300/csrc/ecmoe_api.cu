@@ -151,6 +151,17 @@ ec_status upload_groups(ec_ctx* c) {
   return EC_OK;
 }
 
+// What the kernels expect in a new workspace before the first call.
+ec_status prepare_workspace(ec_ctx* c) {
+  EC_CUDA(cudaMemset(c->ws + c->o_status, 0, 256), "clear status");
+  if (c->bal.G) EC_TRY(balance_upload(c, c->bal));
+  EC_TRY(linear_clear(c));
+  if (c->kind == CTX_EC || c->kind == CTX_TC) EC_TRY(upload_groups(c));
+  // calls on streams that do not wait for this one find all of it there
+  EC_CUDA(cudaStreamSynchronize(cudaStreamLegacy), "prepare the workspace");
+  return EC_OK;
+}
+
 // ---------------------------------------------------------------- SIMT GEMM helper
 // One fp32 product over a batch: operand and output pointers with their batch strides and the
 // stride of the dimension that is not contiguous (a_kfast / b_kfast: contiguous along K).
@@ -753,13 +764,10 @@ ec_status ec_ctx_set_workspace(ec_ctx* c, void* ws, size_t bytes) {
   c->ws = static_cast<char*>(ws);
   c->ws_bytes = bytes;
   c->have_fwd = false;
-  EC_CUDA(cudaMemset(c->ws + c->o_status, 0, 256), "clear status");
-  if (c->bal.G) EC_TRY(balance_upload(c, c->bal));
-  EC_TRY(linear_clear(c));
-  if (c->kind == CTX_EC || c->kind == CTX_TC) EC_TRY(upload_groups(c));
-  // calls on streams that do not wait for this one find all of it there
-  EC_CUDA(cudaStreamSynchronize(cudaStreamLegacy), "prepare the workspace");
-  return EC_OK;
+  const ec_status s = prepare_workspace(c);
+  // kernels follow the tables in it and count its tickets: half prepared it is none
+  if (s != EC_OK) c->ws = nullptr;
+  return s;
 }
 
 ec_status ec_route(ec_ctx* c, const void* X, const void* Wr, const float* br, const float* S_in,
