@@ -67,7 +67,6 @@ class BalanceLoss(Context):
         self.device = torch.device(device)
         self.ctx = ec_balance_ctx_create(self.N, self.E, self.k, group_off)
         self._attach()
-        self.device = self.ws.device
 
     def forward(self, S, choice, mask=None, stream=None):
         """S [N][E] f32 scores, choice [N][k] int32, mask [N] uint8 (0: token left out). Returns (loss [1]
@@ -127,7 +126,6 @@ class Linear(Context):
         self.ctx = ec_linear_ctx_create(self.rows, self.K, self.N, EC_ACTIVATIONS[act], self.code,
                                         self.train)
         self._attach()
-        self.device = self.ws.device
 
     def _rows(self, X):
         m = X.shape[0]

@@ -38,11 +38,14 @@ class Context:
 
     def _attach(self):
         """Allocate the workspace the context asks for and attach it, once what is queued on the current
-        stream and may still use its memory is done."""
-        self.ws_bytes = ec_workspace_bytes(self.ctx)
-        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
-        torch.cuda.current_stream(self.ws.device).synchronize()
-        ec_ctx_set_workspace(self.ctx, self.ws.data_ptr(), self.ws_bytes)
+        stream and may still use its memory is done. The workspace before it is given back first; until
+        the new one is attached ws_bytes is 0."""
+        self.ws, self.ws_bytes = None, 0
+        nbytes = ec_workspace_bytes(self.ctx)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        torch.cuda.current_stream(ws.device).synchronize()
+        ec_ctx_set_workspace(self.ctx, ws.data_ptr(), nbytes)
+        self.ws, self.ws_bytes, self.device = ws, nbytes, ws.device
 
     def _call(self, fn, tensors, stream):
         """One C call: context, the tensors' addresses (None: NULL), the stream."""
@@ -60,11 +63,11 @@ class Context:
         allocates a larger workspace; make it outside stream capture, and capture anew the graphs of
         earlier calls, which hold the old workspace."""
         if p > 0:
-            check_tensor("rng", rng, (2,), torch.int64, self.ws.device)
+            check_tensor("rng", rng, (2,), torch.int64, self.device)
         ec_ctx_set_dropout(self.ctx, p, rng.data_ptr() if p > 0 else None, site)
         self._rng = rng   # the context remembers its address
         if ec_workspace_bytes(self.ctx) > self.ws_bytes:
-            torch.cuda.synchronize(self.ws.device)   # no earlier call may still use the old one
+            torch.cuda.synchronize(self.device)   # no earlier call may still use the old one
             self._attach()
 
     def set_profiling(self, on: bool):
@@ -221,7 +224,7 @@ class TCMoELayer(ECMoELayer):
         """From the next forward on, forward() writes balance_loss [1] and balance_count [G][E] and
         backward() adds the gradient of coef * loss. mask: uint8 [N], 0 for tokens left out."""
         if mask is not None:
-            check_tensor("mask", mask, (self.N,), torch.uint8, self.ws.device)
+            check_tensor("mask", mask, (self.N,), torch.uint8, self.device)
         ec_tc_balance(self.ctx, coef, None if mask is None else mask.data_ptr(),
                       None if self.balance_loss is None else self.balance_loss.data_ptr(),
                       None if self.balance_count is None else self.balance_count.data_ptr())
