@@ -308,8 +308,10 @@ ec_status ec_dropout(int32_t dtype, int64_t n, const void* X, const void* R, voi
  * it is dropped. Dense product: Y = R + drop(act(X W + b)). rng (device, {seed, step}) is remembered
  * and must stay valid; it must hold the same values in the backward call as in the forward call. The
  * first call with p > 0 may raise ec_workspace_bytes, and then detaches an attached workspace (the
- * caller attaches one of the new size); later ones may change p, rng and site, and p = 0 turns dropout
- * off.
+ * caller attaches one of the new size): it waits for the whole device, reads back capacities set by
+ * ec_ctx_set_capacity_async and a status that ec_check_device has not reported yet, and the next
+ * ec_ctx_set_workspace writes both into the new one (call outside stream capture: EC_ERR_CUDA, and
+ * nothing changes). Later calls may change p, rng and site, and p = 0 turns dropout off.
  * Invalidates saved forward state. EC_ERR_STATE on a balance context. */
 ec_status ec_ctx_set_dropout(ec_ctx* ctx, double p, const uint64_t* rng, uint32_t site);
 

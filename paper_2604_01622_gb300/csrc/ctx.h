@@ -87,6 +87,7 @@ struct ec_ctx {
   ecmoe::DropArgs drop;
   bool drop_buf = false;
   size_t o_drop = 0;
+  int kept_status = 0;   // device status word of a workspace given up before anyone read it
   std::string err;
   ec_status err_status = EC_OK;   // status of the last failed call (ec_get_last_error)
 };

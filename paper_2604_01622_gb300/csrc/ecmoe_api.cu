@@ -154,12 +154,34 @@ ec_status upload_groups(ec_ctx* c) {
 // What the kernels expect in a new workspace before the first call.
 ec_status prepare_workspace(ec_ctx* c) {
   EC_CUDA(cudaMemset(c->ws + c->o_status, 0, 256), "clear status");
+  if (c->kept_status)
+    EC_CUDA(cudaMemcpy(c->ws + c->o_status, &c->kept_status, 4, cudaMemcpyHostToDevice), "keep status");
   if (c->bal.G) EC_TRY(balance_upload(c, c->bal));
   EC_TRY(linear_clear(c));
   if (c->kind == CTX_EC || c->kind == CTX_TC) EC_TRY(upload_groups(c));
   // calls on streams that do not wait for this one find all of it there
   EC_CUDA(cudaStreamSynchronize(cudaStreamLegacy), "prepare the workspace");
   return EC_OK;
+}
+
+// What calls have left in the workspace and no host copy holds, before another one takes its place: the
+// status word that nothing has read yet and capacities set from device memory.
+ec_status keep_device_state(ec_ctx* c) {
+  EC_CUDA(cudaDeviceSynchronize(), "wait before another workspace");
+  int word = 0;
+  std::vector<int32_t> k_g(c->kind == CTX_EC ? c->G : 0);
+  EC_CUDA(cudaMemcpy(&word, c->ws + c->o_status, 4, cudaMemcpyDeviceToHost), "read status");
+  if (c->kind == CTX_EC)
+    EC_CUDA(cudaMemcpy(k_g.data(), at<int>(c, c->o_kg), k_g.size() * 4, cudaMemcpyDeviceToHost),
+            "read k_g");
+  if (c->kind == CTX_EC) EC_TRY(set_groups(c, nullptr, k_g.data(), false));
+  c->kept_status = word;
+  return EC_OK;
+}
+
+void set_drop_buf(ec_ctx* c, bool on) {
+  c->drop_buf = on;
+  c->kind == CTX_LINEAR ? block_layout(c) : layout(c);
 }
 
 // ---------------------------------------------------------------- SIMT GEMM helper
@@ -767,6 +789,7 @@ ec_status ec_ctx_set_workspace(ec_ctx* c, void* ws, size_t bytes) {
   const ec_status s = prepare_workspace(c);
   // kernels follow the tables in it and count its tickets: half prepared it is none
   if (s != EC_OK) c->ws = nullptr;
+  else c->kept_status = 0;
   return s;
 }
 
@@ -1030,10 +1053,14 @@ ec_status ec_ctx_set_dropout(ec_ctx* c, double p, const uint64_t* rng, uint32_t 
     if (!rng || (reinterpret_cast<uintptr_t>(rng) & 7u))
       return fail(c, EC_ERR_INVALID_ARG, "rng is required and 8-byte aligned");
     if (!c->drop_buf) {
-      c->drop_buf = true;
       const size_t before = c->total;
-      c->kind == CTX_LINEAR ? block_layout(c) : layout(c);
-      if (c->total != before) c->ws = nullptr;   // laid out for the context without it
+      set_drop_buf(c, true);
+      if (c->ws && c->total != before) {   // laid out for the context without it
+        set_drop_buf(c, false);
+        EC_TRY(keep_device_state(c));
+        set_drop_buf(c, true);
+        c->ws = nullptr;
+      }
     }
     d.rng = reinterpret_cast<const unsigned long long*>(rng);
     d.site = site;

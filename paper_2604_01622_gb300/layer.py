@@ -60,8 +60,9 @@ class Context:
     def set_dropout(self, p, rng=None, site=0):
         """Dropout on the output before the residual (p = 0: off). rng: int64 device tensor {seed, step},
         read by every forward and backward call. The first call with p > 0 waits for the device and
-        allocates a larger workspace; make it outside stream capture, and capture anew the graphs of
-        earlier calls, which hold the old workspace."""
+        allocates a larger workspace (capacities set from device memory and a status not yet checked carry
+        over); make it outside stream capture, and capture anew the graphs of earlier calls, which hold
+        the old workspace."""
         if p > 0:
             check_tensor("rng", rng, (2,), torch.int64, self.device)
         ec_ctx_set_dropout(self.ctx, p, rng.data_ptr() if p > 0 else None, site)
