@@ -121,8 +121,23 @@ def _check(ctx, status: int):
         raise ECError(status, msg)
 
 
+def _fits(lo, hi, **values):
+    """ctypes cuts integers off at their 32 bits; ValueError for those that do not fit."""
+    for name, v in values.items():
+        if not lo <= v < hi:
+            raise ValueError(f"{name}: {v} is not in [{lo}, {hi})")
+
+
+def check_site(site):
+    if not 0 <= site < 1 << 32:
+        raise ValueError(f"site: {site} is not in [0, 2^32)")
+
+
 def _i32(a):
-    arr = np.ascontiguousarray(np.asarray(a, dtype=np.int32))
+    a = np.asarray(a)
+    if a.dtype.kind in "iu" and a.dtype != np.int32 and a.size:
+        _fits(-1 << 31, 1 << 31, smallest=a.min(), largest=a.max())
+    arr = np.ascontiguousarray(a, dtype=np.int32)
     return arr, arr.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
 
 
@@ -271,17 +286,21 @@ def ec_capacity_schedule(scheduler, k_min, k_max, E, group_off, r, sigma=0.22):
 
 def ec_dropout(dtype, n, X, R, Y, p, rng, site, stream):
     """Y = R + drop(X) over n elements (device pointers; R None: 0)."""
+    _fits(-1 << 63, 1 << 63, n=n)
+    check_site(site)
     st = load().ec_dropout(dtype, n, X, R, Y, float(p), rng, int(site), stream)
     if st != EC_OK:
         raise ECError(st, "ec_dropout rejected the call")
 
 
 def ec_ctx_set_dropout(ctx, p, rng, site):
+    check_site(site)
     _check(ctx, load().ec_ctx_set_dropout(ctx, float(p), rng, int(site)))
 
 
 def ec_balance_ctx_create(N, E, k, group_off):
     """Balance-loss context over N tokens in len(group_off) - 1 sequences."""
+    _fits(-1 << 31, 1 << 31, N=N, E=E, k=k)
     ctx = ctypes.c_void_p()
     g_arr, g_ptr = _i32(group_off)
     st = load().ec_balance_ctx_create(ctypes.byref(ctx), N, E, k, len(g_arr) - 1, g_ptr)
@@ -312,6 +331,7 @@ def ec_tc_balance(ctx, coef, mask, loss, count):
 
 def ec_linear_ctx_create(rows, K, N, act, dtype, train=True):
     """Dense-product context: up to `rows` rows, W [K][N], activation code `act`."""
+    _fits(-1 << 31, 1 << 31, rows=rows, K=K, N=N)
     ctx = ctypes.c_void_p()
     st = load().ec_linear_ctx_create(ctypes.byref(ctx), rows, K, N, act, dtype, 1 if train else 0)
     if st != EC_OK:
@@ -320,10 +340,12 @@ def ec_linear_ctx_create(rows, K, N, act, dtype, train=True):
 
 
 def ec_linear_forward(ctx, rows, X, W, b, R, P, Y, stream):
+    _fits(-1 << 31, 1 << 31, rows=rows)
     _check(ctx, load().ec_linear_forward(ctx, rows, X, W, b, R, P, Y, stream))
 
 
 def ec_linear_backward(ctx, rows, dY, X, W, P, dX, dW, db, stream):
+    _fits(-1 << 31, 1 << 31, rows=rows)
     _check(ctx, load().ec_linear_backward(ctx, rows, dY, X, W, P, dX, dW, db, stream))
 
 

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import torch
 
-from . import (EC_ACTIVATIONS, EC_OK, ECError, _check, ec_balance_ctx_create,
+from . import (EC_ACTIVATIONS, EC_OK, ECError, _check, check_site, ec_balance_ctx_create,
                ec_linear_ctx_create, load)
 from .layer import _DT, Context, check_tensor
 
@@ -37,6 +37,7 @@ def dropout(X, p, rng, site=0, R=None, Y=None, stream=None):
     if stream is not None:
         with torch.cuda.stream(stream):
             return dropout(X, p, rng, site, R, Y)
+    check_site(site)
     dev = X.device
     if X.dtype not in _CODE or not X.is_contiguous() or dev.type != "cuda":
         raise ValueError(f"X: a contiguous bf16 or f32 CUDA tensor is wanted, got {X.dtype} on {dev}, "
