@@ -1462,29 +1462,27 @@ cudaError_t launch(const CUtensorMap& a0, const CUtensorMap& a1, const CUtensorM
   constexpr uint32_t smem = smem_bytes<BN, STAGES, PAIR, EPW, EPI>();
   static_assert(smem <= 232448, "dynamic shared memory above the 227 KB per-block limit");
   constexpr int threads = 64 + 32 * EPW;
-  static bool attr = false;
-  static int max_clusters = 0;
-  if (!attr) {
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-    if (PAIR) {
-      cudaLaunchAttribute cl[1];
-      cl[0].id = cudaLaunchAttributeClusterDimension;
-      cl[0].val.clusterDim.x = 2;
-      cl[0].val.clusterDim.y = 1;
-      cl[0].val.clusterDim.z = 1;
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(2 * sm_count());
-      cfg.blockDim = dim3(threads);
-      cfg.dynamicSmemBytes = smem;
-      cfg.attrs = cl;
-      cfg.numAttrs = 1;
-      e = cudaOccupancyMaxActiveClusters(&max_clusters, kern, &cfg);
-      if (e != cudaSuccess) return e;
-      if (max_clusters <= 0) return cudaErrorNotSupported;
-    }
-    attr = true;
-  }
+  static PerDevice once;
+  int max_clusters = 0;   // PAIR: that run at the same time; else 1
+  const cudaError_t e = once.get(&max_clusters, [&](int* most) {
+    cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    *most = 1;
+    if (err != cudaSuccess || !PAIR) return err;
+    cudaLaunchAttribute cl[1];
+    cl[0].id = cudaLaunchAttributeClusterDimension;
+    cl[0].val.clusterDim.x = 2;
+    cl[0].val.clusterDim.y = 1;
+    cl[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * sm_count());
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.attrs = cl;
+    cfg.numAttrs = 1;
+    err = cudaOccupancyMaxActiveClusters(most, kern, &cfg);
+    return err == cudaSuccess && *most <= 0 ? cudaErrorNotSupported : err;
+  });
+  if (e != cudaSuccess) return e;
   // variable rows: p.M carries an upper bound of the padded rows, so `total` bounds the tiles
   if (PAIR) {
     p.m_tiles = (p.M + 2 * BM - 1) / (2 * BM);

@@ -424,12 +424,13 @@ cudaError_t tile_go(const TileProblem<T>& t, int splits, LaunchStream st) {
   constexpr int form = PAIR ? 2 : BN == 128 ? 1 : 0;
   constexpr int PL = kSums<T> ? 3 : 1;
   const int a_rows = tile_a_rows(form, !A_MN, t.M), stage = tile_stage(form, PL, a_rows);
-  static bool attr = false;
-  if (!attr) {
-    TC_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                kTileDeep + kTileExtra));
-    attr = true;
-  }
+  static PerDevice once;
+  int set = 0;
+  TC_TRY(once.get(&set, [&](int* v) {
+    *v = 1;
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                kTileDeep + kTileExtra);
+  }));
   CUtensorMap ma, mb;
   TC_TRY(A_MN ? tile_map(&ma, t.A, t.M, t.K, t.lda, PL, 64)
               : tile_map(&ma, t.A, t.K, t.M, t.lda, PL, a_rows));
