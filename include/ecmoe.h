@@ -327,7 +327,7 @@ ec_status ec_ctx_set_dropout(ec_ctx* ctx, double p, const uint64_t* rng, uint32_
  *   S [N][E] float scores (16-byte aligned); choice [N][k] int32, k <= E: an entry outside [0, E)
  *   counts for no expert, the same expert twice counts twice; mask [N] uint8 (0: token left out,
  *   whatever its scores and choices hold) or NULL; loss [1] float; count [G][E] int32 (NULL: not
- *   written); dloss [1] float, the upstream gradient (NULL: 1); dZ [N][E] float, overwritten, no
+ *   written), no overlap with the inputs or each other; dloss [1] float, the upstream gradient (NULL: 1); dZ [N][E] float, overwritten, no
  *   overlap with the inputs.
  * E <= 512 and N k <= 2^30, else EC_ERR_UNSUPPORTED. A balance context uses ec_workspace_bytes,
  * ec_ctx_set_workspace, profiling, ec_check_device and the error calls as a layer's context does; other

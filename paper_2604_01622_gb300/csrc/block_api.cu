@@ -275,6 +275,13 @@ ec_status ec_balance_forward(ec_ctx* c, const float* S, const int32_t* choice, c
   for (const void* p : {(const void*)choice, (const void*)loss, (const void*)count})
     if (reinterpret_cast<uintptr_t>(p) & 3u)
       return fail(c, EC_ERR_INVALID_ARG, "choice, loss and count must be 4-byte aligned");
+  // sequences are finished while others are still read
+  const size_t N = c->bal.N, E = c->bal.E;
+  const Span out[2] = {{loss, 4}, {count, (size_t)c->bal.G * E * 4}};
+  for (const Span& o : out)
+    if (overlap(o, {S, N * E * 4}) || overlap(o, {choice, N * c->bal.k * 4}) || overlap(o, {mask, N}))
+      return fail(c, EC_ERR_INVALID_ARG, "loss and count may not overlap an input");
+  if (overlap(out[0], out[1])) return fail(c, EC_ERR_INVALID_ARG, "loss may not overlap count");
   const LaunchStream st(static_cast<cudaStream_t>(stream), true);
   BalanceArgs p = balance_args(c, c->bal);
   p.S = S; p.choice = choice; p.mask = mask; p.loss = loss; p.count = count;
