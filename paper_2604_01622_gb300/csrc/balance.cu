@@ -208,13 +208,15 @@ balance_kernel(BalanceArgs p) {
 
 // dZ = dloss S (f' - <S, f'> + f0 (1 - sum S)) with f' = f - f0: the row's mean is taken out first,
 // so that the difference of two nearly equal numbers of f0's size is not formed from rounded ones
-// (with balanced experts f' is a few percent of f0). `lanes` lanes (a power of two) to a token, NV
-// vectors of V experts to a lane; blockIdx.y: the parts of the chunk, each as many tokens as the block has
-// in flight, dealt out to as many CTAs as make eight to an SM (65536 x 128: 13.0 us, a CTA to every part
-// 13.8, four to an SM 14.8).
+// (with balanced experts f' is a few percent of f0, or a few thousandths). So that f0 (1 - sum S) does not
+// err by 2^-24 f0 and more, a score is added up in two parts: what it has in multiples of 2^-22, whose sum
+// is exact up to 4, and the rest, which goes with the small terms (3 to 7% of the time of scores that lie
+// in L2). `lanes` lanes (a power of two) to a token, NV vectors of V experts to a lane; blockIdx.y: the
+// parts of the chunk, each as many tokens as the block has in flight, dealt out to as many CTAs as make
+// eight to an SM (65536 x 128: with a CTA to every part 6% longer, with four to an SM 14%).
 constexpr int kGradThreads = 256, kGradCtas = 8;
 template <int NV>
-constexpr int kGradTokens = NV <= 2 ? 4 : 2;   // tokens a thread has in flight
+constexpr int kGradTokens = NV <= 2 ? 4 : NV <= 4 ? 2 : 1;   // tokens a thread has in flight
 template <int V, int NV, bool MASK>
 __global__ void __launch_bounds__(kGradThreads, 4)
 balance_grad_kernel(BalanceArgs p, const float* dloss, float* dZ, int lanes) {
@@ -253,21 +255,25 @@ balance_grad_kernel(BalanceArgs p, const float* dloss, float* dZ, int lanes) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int t = tb + u * per;
-      float sum = 0.f, dot = 0.f;
+      float sum = 3.f, rest = 0.f, dot = 0.f;   // in [2, 4) sums are multiples of 2^-22
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         if ((j + i * lanes) * V < E)
 #pragma unroll
           for (int q = 0; q < V; ++q) {
-            sum += s[u][i][q];
-            dot = fmaf(s[u][i][q], tab[i][q], dot);
+            const float x = s[u][i][q], next = sum + x;
+            rest += x - (next - sum);
+            sum = next;
+            dot = fmaf(x, tab[i][q], dot);
           }
       }
+      sum -= 3.f;
+      dot = fmaf(f0, rest, dot);
       for (int o = lanes >> 1; o > 0; o >>= 1) {
         sum += __shfl_xor_sync(0xffffffffu, sum, o);
         dot += __shfl_xor_sync(0xffffffffu, dot, o);
       }
-      const float c = f0 * (1.f - sum) - dot;
+      const float c = fmaf(f0, 1.f - sum, -dot);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int e = (j + i * lanes) * V;
@@ -315,8 +321,12 @@ static cudaError_t grad_go(const BalanceArgs& p, const float* dloss, float* dZ, 
   const int tokens = kGradThreads / lanes * kGradTokens<NV>;
   const dim3 grid(p.chunks, std::min((p.chunk_tokens + tokens - 1) / tokens,
                                      (kGradCtas * kSms + p.chunks - 1) / p.chunks));
+  // A grid of one wave of four CTAs to an SM takes shared memory that nobody uses, so that an SM takes no
+  // fifth while another has three (32768 x 64: 3.4 us, without it 3.9; on larger grids it only takes L1
+  // away, 131072 x 128: 22.7 us, without it 21.9).
+  const size_t smem = (int64_t)grid.x * grid.y <= 4 * kSms ? 46 * 1024 : 0;
   auto go = [&](auto kern) {
-    return launch_kernel(kern, grid, kGradThreads, 0, st, 1, p, dloss, dZ, lanes);
+    return launch_kernel(kern, grid, kGradThreads, smem, st, 1, p, dloss, dZ, lanes);
   };
   return p.mask ? go(balance_grad_kernel<V, NV, true>) : go(balance_grad_kernel<V, NV, false>);
 }

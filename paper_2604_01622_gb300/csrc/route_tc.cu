@@ -345,7 +345,9 @@ int64_t tc_route_scratch_ints(int N, int E) {
 // dS_tj = (dg_tj - sum_{j' kept} dg_tj' g_tj') / Z_t for the k chosen j (dg = 0 if dropped),
 // dZ = S * (dS - <dS, S>). dg is the sum of the pair's gate-gradient partials [parts][P], in part
 // order, found through the slot map; lane r < k holds the token's r-th choice. BAL: the token's row of
-// a balance term is added to dS for every expert.
+// a balance term is added to dS for every expert, less its mean, which a softmax's scores, whose sum is 1,
+// do not feel (what their sum strays from 1 by rounding is left out here; balance.cu, for scores of any
+// sum, has it).
 template <bool BAL>
 __global__ void tc_softmax_bwd_kernel(const float* __restrict__ S, const int* __restrict__ choice,
                                       const float* __restrict__ tgate, const float* __restrict__ Z,
