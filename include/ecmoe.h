@@ -360,10 +360,12 @@ ec_status ec_tc_balance(ec_ctx* ctx, float coef, const uint8_t* mask, float* los
  *   is). 0 <= rows <= the context's, a new number each call. K and N up to 2^20, multiples of 8 (bf16)
  *   or 4 (fp32), rows up to 2^23, else EC_ERR_UNSUPPORTED. Y and P overlap neither an input nor each other.
  * Activations: relu; silu x s(x); gelu in its tanh form, x s(2 sqrt(2/pi) (x + 0.044715 x^3)), s the
- * logistic sigmoid. Sums are fp32 in both dtypes. fp32 products of more than 16 rows (small weights: 48),
- * and the backward call's, split each operand into three bf16 parts (what is left out is 2^-22 of a
- * product): an infinite operand, or one above the largest bf16 (3.39e38), gives NaN where IEEE products
- * may give infinities.
+ * logistic sigmoid. Sums are fp32 in both dtypes. bf16 products: the tensor cores cut off what does not fit
+ * when they add, up to 1.7e-4 of a sum of one sign whatever its length, a twentieth of what rounding to bf16
+ * may take. fp32 products of more than 16 rows (small weights: 48), and the backward call's, split each
+ * operand into three bf16 parts (what is left out is 2^-22 of a product); against 64 bits the sum errs by
+ * 3e-7 in the root mean square whatever its length. An infinite operand, or one above the largest bf16
+ * (3.39e38), gives NaN there where IEEE products may give infinities.
  * ec_linear_backward: from dY, with dP = drop(dY) act'(P) (rounded to the dtype before the products):
  *   dX = dP W^T [rows][K], dW = X^T dP [K][N], db = column sums of dP [N]; each NULL to skip, in the
  *   context's dtype, overwritten, no overlap with the inputs or one another. P is what the forward

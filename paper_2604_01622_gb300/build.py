@@ -17,7 +17,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libecmoe.so")
 SOURCES = ["ecmoe_api.cu", "route.cu", "route_tc.cu", "moves.cu", "gemm_simt.cu", "gemm_tc.cu",
            "select_static.cu", "block_api.cu", "dropout.cu", "balance.cu", "linear.cu", "linear_tc.cu",
-           "linear_tile_bf16.cu", "linear_tile_f32.cu", "capacity.cpp"]
+           "linear_tile_bf16.cu", "linear_tile_f32.cu", "linear_tile_long_bf16.cu",
+           "linear_tile_long_f32.cu", "capacity.cpp"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

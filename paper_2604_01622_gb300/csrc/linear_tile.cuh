@@ -95,28 +95,34 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
   return v;
 }
 
-// The tensor cores add in fp32 but cut off what does not fit, so a long sum drifts: 2e-8 of its size for
-// every 16 of K (1.2e-6 at K 1000, 1e-5 at 8192). For fp32 results (SUMS) an accumulator therefore takes
-// one k-slice, in which only the last four steps add numbers of the sum's size, and is then added to sums
-// in registers, rounded to nearest, by eight warps of their own, while the MMAs go on in a second
-// accumulator. Against 64 bits: 1e-7 at K 1000, where the product of fp32 numbers, added one by one, has
-// 5.7e-7.
+// The tensor cores add in fp32 but cut off what does not fit, so a long sum of one sign drifts: up to 1e-7 of
+// its size for every 16 of K (2e-5 at K 8192, 1.7e-4 at 32768, 1.6e-3 at 262144). With SUMS an accumulator therefore takes few k-slices and
+// is then added to sums in registers, rounded to nearest, by eight warps of their own, while the MMAs go
+// on in a second accumulator:
+// - fp32 results, always: one k-slice, in which only the last four steps add numbers of the sum's size.
+//   Against 64 bits 1e-7 at K 1000, where the product of fp32 numbers, added one by one, has 5.7e-7. Above
+//   kBlockSlices k-slices (SUMS 2) the register sums of so many are added up on a second level, so that
+//   neither chain is long: 1e-7 to 2.4e-7 of a sum of one sign from K 1000 to 524288 (one chain of 32768
+//   slices: 1.3e-6).
+// - bf16 results, where an accumulator would take more than kLongSlices (both in linear_tile.h): kLongRun
+//   k-slices, a drift of 2.6e-5 at most, a hundredth of half a bf16 step.
+constexpr int kLongRun = 64;
 template <typename T>
-constexpr bool kSums = sizeof(T) == 4;
-template <typename T>
-constexpr int kTileBlock = kTileThreads + (kSums<T> ? 64 : 0);
+constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+template <int SUMS>
+constexpr int kTileBlock = kTileThreads + (SUMS ? 64 : 0);
 
-template <int BN, bool A_MN, bool B_MN, bool PAIR, typename T>
-__global__ void __launch_bounds__(kTileBlock<T>, kSums<T> ? 1 : 2)
+template <int BN, bool A_MN, bool B_MN, bool PAIR, typename T, int SUMS>
+__global__ void __launch_bounds__(kTileBlock<SUMS>, SUMS ? 1 : 2)
 linear_tile_kernel(const __grid_constant__ CUtensorMap mA, const __grid_constant__ CUtensorMap mB,
                    LinearEpi<T> ep, TileArgs p) {
   constexpr int BNL = PAIR ? BN / 2 : BN;        // columns of B in this CTA's shared memory
   constexpr int NP = PAIR ? 2 : 1;
-  constexpr int PL = kSums<T> ? 3 : 1;           // planes of an operand
+  constexpr int PL = kPlanes<T>;                 // of an operand
+  constexpr int RUN = PL == 3 ? 1 : kLongRun;    // SUMS: k-slices an accumulator takes
   constexpr uint32_t B_BYTES = BNL * BK * 2;     // of one plane's slice
   const uint32_t a_bytes = (uint32_t)p.a_rows * BK * 2;
   constexpr uint32_t IDESC = instr_desc<BN, A_MN, B_MN, NP * BM>();
-  constexpr bool SUMS = kSums<T>;
   constexpr int FIRST = SUMS ? 2 : 0;            // the first warp of the eight that finish the tile
   constexpr uint32_t TCOLS = SUMS ? 2 * BN : BN;
   extern __shared__ uint8_t smem_raw[];
@@ -230,35 +236,62 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mA, const __grid_constant
       };
       const uint32_t da0 = desc_lo(smem_u32(sA), A_MN ? 8192 : 16);
       const uint32_t db0 = desc_lo(smem_u32(sB), B_MN ? 8192 : 16);
-      int s = 0, a = 0;   // SUMS: a the accumulator of the slice
-      uint32_t ph = 0, acc = 0, free_ph = 1;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (SUMS && !mbar_wait_warp(&tempty[a], free_ph, abort_flag, p.status)) break;
-        const uint32_t d = tmem + (SUMS ? a * BN : 0);
-        if (!mbar_wait_warp(&full[s], ph, abort_flag, p.status)) break;
-        tc_fence_after();
+      int s = 0;
+      uint32_t ph = 0;
+      // the MMAs of ring slot s into accumulator d, which starts from zero where acc is 0
+      auto issue = [&](uint32_t d, uint32_t acc) {
         const uint32_t a0 = da0 + s * PL * (a_bytes >> 4), b0 = db0 + s * PL * (B_BYTES >> 4);
-        if (one) {
 #pragma unroll
-          for (int g = 0; g < (SUMS ? 6 : 1); ++g) {
-            const uint32_t ag = SUMS ? a0 + kPlaneA[g] * (a_bytes >> 4) : a0;
-            const uint32_t bg = SUMS ? b0 + kPlaneB[g] * (B_BYTES >> 4) : b0;
+        for (int g = 0; g < (PL == 3 ? 6 : 1); ++g) {
+          const uint32_t ag = PL == 3 ? a0 + kPlaneA[g] * (a_bytes >> 4) : a0;
+          const uint32_t bg = PL == 3 ? b0 + kPlaneB[g] * (B_BYTES >> 4) : b0;
 #pragma unroll
-            for (int j = 0; j < BK / 16; ++j) {
-              const uint32_t ad = ag + j * (A_MN ? 2048 >> 4 : 32 >> 4);
-              const uint32_t bd = bg + j * (B_MN ? 2048 >> 4 : 32 >> 4);
-              const uint32_t on = g + j == 0 ? (SUMS ? 0u : acc) : 1u;
-              if constexpr (PAIR) mma_bf16_pair(d, ad, bd, IDESC, on);
-              else mma_bf16(d, ad, bd, IDESC, on);
-            }
+          for (int j = 0; j < BK / 16; ++j) {
+            const uint32_t ad = ag + j * (A_MN ? 2048 >> 4 : 32 >> 4);
+            const uint32_t bd = bg + j * (B_MN ? 2048 >> 4 : 32 >> 4);
+            const uint32_t on = g + j == 0 ? acc : 1u;
+            if constexpr (PAIR) mma_bf16_pair(d, ad, bd, IDESC, on);
+            else mma_bf16(d, ad, bd, IDESC, on);
           }
-          commit(&empty[s]);
-          if (SUMS) commit(&tfull[a]);
         }
-        __syncwarp();
-        acc = 1;
-        if (SUMS && (a ^= 1) == 0) free_ph ^= 1u;
-        if (++s == p.stages) { s = 0; ph ^= 1u; }
+        commit(&empty[s]);
+      };
+      if constexpr (SUMS == 0 || RUN == 1) {
+        int a = 0;   // SUMS: the accumulator of the slice
+        uint32_t acc = 0, free_ph = 1;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (SUMS && !mbar_wait_warp(&tempty[a], free_ph, abort_flag, p.status)) break;
+          if (!mbar_wait_warp(&full[s], ph, abort_flag, p.status)) break;
+          tc_fence_after();
+          if (one) {
+            issue(tmem + (SUMS ? a * BN : 0), SUMS ? 0u : acc);
+            if (SUMS) commit(&tfull[a]);
+          }
+          __syncwarp();
+          acc = 1;
+          if (SUMS && (a ^= 1) == 0) free_ph ^= 1u;
+          if (++s == p.stages) { s = 0; ph ^= 1u; }
+        }
+      } else {
+        // a loop over the slices of an accumulator as short as the one without register sums: with the
+        // accumulator changing inside it a slice of 128 x 64 tiles took 0.226 us, so 0.172, as without
+        bool good = true;
+        for (int kb = kb0, c = 0; kb < kb1 && good; ++c) {
+          const int end = min(kb + RUN, kb1);
+          good = mbar_wait_warp(&tempty[c & 1], (uint32_t)(c >> 1 & 1) ^ 1u, abort_flag, p.status);
+          const uint32_t d = tmem + (c & 1) * BN;
+          uint32_t acc = 0;
+          for (; kb < end && good; ++kb) {
+            if (!mbar_wait_warp(&full[s], ph, abort_flag, p.status)) { good = false; break; }
+            tc_fence_after();
+            if (one) issue(d, acc);
+            __syncwarp();
+            acc = 1;
+            if (++s == p.stages) { s = 0; ph ^= 1u; }
+          }
+          if (one) commit(&tfull[c & 1]);
+          __syncwarp();
+        }
       }
       // also where the loop gave up: the MMAs already issued end before TMEM is released
       if (one) commit(done);
@@ -266,12 +299,26 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mA, const __grid_constant
     }
     // the other warps wait at the barrier below, where they take no issue slots from the two at work
     mbar_wait_warp(done, 0, abort_flag, p.status);
-  } else if constexpr (SUMS) {
+  } else if constexpr (SUMS != 0) {
+    float blocks[SUMS == 2 ? BN / 64 : 1][32];   // SUMS 2: what is closed of the sum
+    auto close_block = [&] {
+#pragma unroll
+      for (int i = 0; i < BN / 64; ++i)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          blocks[i][j] += sum[i][j];
+          sum[i][j] = 0.f;
+        }
+    };
 #pragma unroll
     for (int i = 0; i < BN / 64; ++i)
 #pragma unroll
-      for (int j = 0; j < 32; ++j) sum[i][j] = 0.f;
-    for (int c = 0; c < kb1 - kb0; ++c) {
+      for (int j = 0; j < 32; ++j) {
+        sum[i][j] = 0.f;
+        if (SUMS == 2) blocks[i][j] = 0.f;
+      }
+    const int runs = (kb1 - kb0 + RUN - 1) / RUN;
+    for (int c = 0; c < runs; ++c) {
       const int a = c & 1;
       if (!mbar_wait_warp(&tfull[a], (uint32_t)(c >> 1) & 1u, abort_flag, p.status)) break;
       tc_fence_after();
@@ -286,6 +333,15 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap mA, const __grid_constant
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&tempty[a]), rank & ~(uint32_t)(NP - 1)));
+      if constexpr (SUMS == 2)
+        if (c % kBlockSlices == kBlockSlices - 1) close_block();
+    }
+    if constexpr (SUMS == 2) {
+      close_block();
+#pragma unroll
+      for (int i = 0; i < BN / 64; ++i)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) sum[i][j] = blocks[i][j];
     }
   }
   tc_fence_before();
@@ -418,12 +474,11 @@ cudaError_t tile_map(CUtensorMap* m, const void* base, uint64_t cols, uint64_t r
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int BN, bool A_MN, bool B_MN, bool PAIR, typename T>
-cudaError_t tile_go(const TileProblem<T>& t, int splits, LaunchStream st) {
-  auto kern = linear_tile_kernel<BN, A_MN, B_MN, PAIR, T>;
-  constexpr int form = PAIR ? 2 : BN == 128 ? 1 : 0;
-  constexpr int PL = kSums<T> ? 3 : 1;
-  const int a_rows = tile_a_rows(form, !A_MN, t.M), stage = tile_stage(form, PL, a_rows);
+template <int BN, bool A_MN, bool B_MN, bool PAIR, int SUMS, typename T>
+cudaError_t tile_go(const TileProblem<T>& t, const TileChoice& c, LaunchStream st) {
+  auto kern = linear_tile_kernel<BN, A_MN, B_MN, PAIR, T, SUMS>;
+  constexpr int PL = kPlanes<T>;
+  const int a_rows = tile_a_rows(c.form, !A_MN, t.M), stage = tile_stage(c.form, PL, a_rows);
   static PerDevice once;
   int set = 0;
   TC_TRY(once.get(&set, [&](int* v) {
@@ -439,36 +494,39 @@ cudaError_t tile_go(const TileProblem<T>& t, int splits, LaunchStream st) {
   TileArgs p;
   p.M = t.M; p.N = t.N;
   p.blocks = (t.K + BK - 1) / BK;
-  p.splits = splits;
+  p.splits = c.splits;
   p.n_tiles = (t.N + BN - 1) / BN;
   p.status = t.status;
-  const int rows = PAIR ? 2 * BM : BM, cluster = splits * (PAIR ? 2 : 1);
+  const int rows = PAIR ? 2 * BM : BM, cluster = c.splits * (PAIR ? 2 : 1);
   const int64_t ctas = (int64_t)((t.M + rows - 1) / rows) * p.n_tiles * cluster;
-  p.stages = tile_ring(stage, kSums<T> || tile_deep(ctas, cluster));
+  p.stages = tile_ring(stage, SUMS || tile_deep(ctas, cluster));
   p.a_rows = a_rows;
   p.beside = t.beside;
   // the ring holds the sums afterwards, and the MMA's reads past the last rows of A end inside it
   const int sums = std::min(t.M, BM) * BN * 4;
   const int ring = std::max({p.stages * stage, sums, (p.stages * PL - 1) * a_rows * 128 + BM * 128});
-  return launch_kernel(kern, (unsigned)ctas, kTileBlock<T>, (size_t)ring + kTileExtra, st, cluster, ma,
+  return launch_kernel(kern, (unsigned)ctas, kTileBlock<SUMS>, (size_t)ring + kTileExtra, st, cluster, ma,
                        mb, t.ep, p);
 }
 
-template <bool A_MN, bool B_MN, typename T>
+// The last form of kTileForms is for long sums of bf16 products alone.
+template <bool A_MN, bool B_MN, int SUMS, typename T>
 cudaError_t tile_form(const TileProblem<T>& t, const TileChoice& c, LaunchStream st) {
   switch (c.form) {
-    case 0: return tile_go<64, A_MN, B_MN, false, T>(t, c.splits, st);
-    case 1: return tile_go<128, A_MN, B_MN, false, T>(t, c.splits, st);
+    case 0: return tile_go<64, A_MN, B_MN, false, SUMS>(t, c, st);
+    case 1: return tile_go<128, A_MN, B_MN, false, SUMS>(t, c, st);
+    case 2: return tile_go<128, A_MN, B_MN, true, SUMS>(t, c, st);
   }
-  return tile_go<128, A_MN, B_MN, true, T>(t, c.splits, st);
+  if constexpr (sizeof(T) == 2 && SUMS) return tile_go<256, A_MN, B_MN, true, SUMS>(t, c, st);
+  return cudaErrorInvalidValue;
 }
 
-template <typename T>
+template <int SUMS, typename T>
 cudaError_t tile_launch(const TileProblem<T>& t, const TileChoice& c, LaunchStream st) {
   switch (t.form) {
-    case LIN_FWD: return tile_form<false, true, T>(t, c, st);
-    case LIN_DX: return tile_form<false, false, T>(t, c, st);
-    case LIN_DW: return tile_form<true, true, T>(t, c, st);
+    case LIN_FWD: return tile_form<false, true, SUMS>(t, c, st);
+    case LIN_DX: return tile_form<false, false, SUMS>(t, c, st);
+    case LIN_DW: return tile_form<true, true, SUMS>(t, c, st);
   }
   return cudaErrorInvalidValue;
 }

@@ -1,5 +1,7 @@
 // Which kernel and form a dense product takes, by estimated time. Internal.
 #pragma once
+#include <cuda_bf16.h>
+
 #include <algorithm>
 #include <cstdint>
 
@@ -7,13 +9,15 @@
 
 namespace ecmoe {
 
-// Forms of linear_tile.cuh: one-CTA tiles of 128 x 64 and 128 x 128, pair tiles of 256 x 128. (Pair tiles of
-// 256 x 256, too, were the fastest at none of 65 products: where they are many, the persistent kernel is.)
+// Forms of linear_tile.cuh: one-CTA tiles of 128 x 64 and 128 x 128, pair tiles of 256 x 128; for long sums
+// pair tiles of 256 x 256. (Those were the fastest at none of 65 other products: where they are many, the
+// persistent kernel is.)
 struct TileForm {
   int rows, cols, ctas;   // of a tile; CTAs that work on one block of K
-  double planes_us;       // the least a k-slice of fp32 planes, 24 MMAs, takes
+  double planes_us;       // the least a k-slice of fp32 planes, 24 MMAs, takes; 256 x 256: six times four
 };
-constexpr TileForm kTileForms[3] = {{128, 64, 1, 0.8}, {128, 128, 1, 1.1}, {256, 128, 2, 0.92}};
+constexpr TileForm kTileForms[4] = {{128, 64, 1, 0.8}, {128, 128, 1, 1.1}, {256, 128, 2, 0.92},
+                                    {256, 256, 2, 1.7}};
 
 // Rows of A that a CTA loads: of a product of fewer than 128 rows only those there are, in eights (the
 // swizzle's unit), where they are rows in memory. The MMA still reads 128: what stands in the others' place
@@ -41,6 +45,17 @@ struct TileChoice {
   double us;
 };
 
+// Which products: bf16 operands, fp32 ones as three planes, or bf16 ones with a sum too long for one
+// accumulator. The last two keep the tile's sums in registers (SUMS in linear_tile.cuh).
+enum TileKind { TILE_BF16, TILE_F32, TILE_LONG };
+// k-slices that an accumulator of bf16 operands takes at most, 32768 of K: what the tensor cores cut off of a
+// sum of one sign is 1.7e-4 of it then, a twentieth of half a bf16 step.
+constexpr int64_t kLongSlices = 512;
+// k-slices whose fp32 results are added in one chain; a power of two. (1000 x 500 x 364: 12.7 us, with the
+// second level's registers 13.6.)
+constexpr int kBlockSlices = 256;
+inline int64_t tile_chain(int64_t slices, int splits) { return (slices + splits - 1) / splits; }
+
 // The form and the number of blocks of K with the least estimated time. A CTA's k-slice takes a share of a
 // load's round trip (1.42 us over the slices of the ring) or its bytes at 139 GB/s an SM from L2, whichever
 // is longer, and its epilogue 0.09 us per 1000 outputs; a tile's joined blocks 0.093 us per 1000 of all of
@@ -48,20 +63,27 @@ struct TileChoice {
 // 8192), of which it takes the fastest form or one 2% slower on average, a quarter at worst. fp32 results
 // (f32): one CTA to an SM, whose registers hold the tile's sums, clusters of four at most, and three planes
 // an operand (19 products: the fastest form or one 2% slower at worst).
-inline TileChoice tile_choice(bool f32, bool a_rows, int64_t M, int64_t N, int64_t slices) {
+// Long sums: one CTA to an SM likewise, and split only where all their CTAs run at once (100000 rows of
+// 2048 x 8192, 512 CTAs: dW 2.05 ms, split in two 2.20), into eight where there are no more than eight tiles
+// (2097152 rows of 64 x 64: 710 us, in four 1400; 16 tiles and more: half as long again in eight as in four).
+inline TileChoice tile_choice(TileKind kind, bool a_rows, int64_t M, int64_t N, int64_t slices) {
   TileChoice best{0, 1, 1e30};
-  for (int f = 0; f < 3; ++f) {
+  const bool sums = kind != TILE_BF16;
+  for (int f = 0; f < (kind == TILE_LONG ? 4 : 3); ++f) {
     const TileForm& t = kTileForms[f];
     const int64_t tiles = ((M + t.rows - 1) / t.rows) * ((N + t.cols - 1) / t.cols);
-    const int stage = tile_stage(f, f32 ? 3 : 1, tile_a_rows(f, a_rows, M));
-    for (int s = 1; s * t.ctas <= (f32 ? 4 : 8) && s <= slices; s *= 2) {
+    const int stage = tile_stage(f, kind == TILE_F32 ? 3 : 1, tile_a_rows(f, a_rows, M));
+    const int most = kind == TILE_BF16 || (kind == TILE_LONG && tiles <= 8) ? 8 : 4;
+    for (int s = 1; s * t.ctas <= most && s <= slices; s *= 2) {
       const int64_t ctas = tiles * t.ctas * s;
-      const bool deep = f32 || tile_deep(ctas, t.ctas * s);
+      if (kind == TILE_BF16 && tile_chain(slices, s) > kLongSlices) continue;
+      if (kind == TILE_LONG && s > 1 && ctas > kSms) continue;
+      const bool deep = sums || tile_deep(ctas, t.ctas * s);
       const int on = deep ? 1 : 2;   // CTAs an SM runs at once
       const int64_t turns = (ctas + kSms * on - 1) / (kSms * on);
       const double at_once = (double)std::min<int64_t>(on, (ctas + kSms - 1) / kSms);
       const double slice = std::max({1.42 / tile_ring(stage, deep), at_once * stage / 139e3,
-                                     f32 ? t.planes_us : 0.0});
+                                     !sums ? 0.0 : kind == TILE_F32 ? t.planes_us : t.planes_us / 6});
       const double outputs = std::min<double>((double)M, 128.0) * t.cols / 1000;
       const double finish = s == 1 ? 0.09 * outputs : 1.1 + 0.093 * outputs;
       const double us =
@@ -72,8 +94,14 @@ inline TileChoice tile_choice(bool f32, bool a_rows, int64_t M, int64_t N, int64
   return best;
 }
 
-// The persistent kernel's 256 x 256 pair tiles: 0.275 us a k-slice and wave of tiles (64 tiles of 32 slices:
-// 15.7 us, of 128: 42.0 us; pair tiles of 256 x 128: 16.3 and 44.5 us).
+// The tile kernel for sums too long for one accumulator (bf16) or one chain of fp32 sums, in a chosen form.
+template <typename T>
+struct TileProblem;
+cudaError_t tc_linear_long(const TileProblem<__nv_bfloat16>& t, const TileChoice& c, LaunchStream st);
+cudaError_t tc_linear_long(const TileProblem<float>& t, const TileChoice& c, LaunchStream st);
+
+// The persistent kernel's 256 x 256 pair tiles, for sums that one accumulator takes: 0.275 us a k-slice and
+// wave of tiles (64 tiles of 32 slices: 15.7 us, of 128: 42.0 us; pair tiles of 256 x 128: 16.3 and 44.5 us).
 inline double pairs_us(int64_t M, int64_t N, int64_t slices) {
   const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), walkers = kSms / 2;
   return 6.8 + 0.275 * (double)((tiles + walkers - 1) / walkers) * (double)slices;
