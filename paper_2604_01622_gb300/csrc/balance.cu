@@ -88,7 +88,7 @@ balance_kernel(BalanceArgs p) {
       // all loads of a round without a condition, the chunk's last token again past its end, so that
       // they are in flight together; a masked token's scores are left out when they are added
       float x[U][V];
-      uint32_t use[U];   // all ones or 0: a selection would draw the loads behind its condition
+      uint32_t use[U];   // all ones or 0
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int tu = min(t + u * rows, t1 - 1);

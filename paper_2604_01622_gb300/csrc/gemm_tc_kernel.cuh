@@ -145,9 +145,8 @@ __device__ __noinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile 
   }
 }
 // The same by a whole warp, with one answer for all lanes and the first look at the barrier in line (most
-// waits of a main loop find it complete). The loops around it stay uniform, so that the compiler keeps
-// addresses and descriptors in uniform registers: in a branch of one lane every operand of a tensor-core
-// or TMA instruction was moved there anew, which made a k-slice 500 clocks at least.
+// waits of a main loop find it complete). The loops around it are the whole warp's, and an elected lane
+// issues inside them: with the loop in a branch of one lane a k-slice took 500 clocks at least.
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
                                                int* status) {
   if (__all_sync(0xffffffffu, mbar_try_wait(smem_u32(bar), parity))) return true;

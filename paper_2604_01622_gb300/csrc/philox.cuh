@@ -30,8 +30,8 @@ __device__ __forceinline__ DropKey drop_key(const DropArgs& d) {
 constexpr uint32_t kPhiloxM0 = 0xD2511F53u, kPhiloxM1 = 0xCD9E8D57u;   // multipliers
 constexpr uint32_t kPhiloxW0 = 0x9E3779B9u, kPhiloxW1 = 0xBB67AE85u;   // key increments
 
-// Both halves of a product in one instruction (written in C++ they came out as two; dropout of 67 M bf16
-// values and its gradient 125 -> 113 us).
+// Both halves of a product (dropout of 67 M bf16 values and its gradient 113 us; with a 64-bit product in C++,
+// shifted and cut, 125).
 __device__ __forceinline__ void mul_wide(uint32_t m, uint32_t x, uint32_t& hi, uint32_t& lo) {
   asm("{\n\t.reg .b64 t;\n\tmul.wide.u32 t, %2, %3;\n\tmov.b64 {%0, %1}, t;\n\t}"
       : "=r"(lo), "=r"(hi)
