@@ -24,6 +24,7 @@ import hashlib
 import json
 import math
 import os
+import re
 import subprocess
 import sys
 import tempfile
@@ -38,9 +39,11 @@ UNIT = "tokens/s"
 
 # DRAM traffic per launch of the grouped-GEMM kernels (dram__bytes_read.sum +
 # dram__bytes_write.sum, mean of the six expert-GEMM launches of one step), keyed by the hash
-# of the kernel source it was taken on; a changed kernel reports null until re-captured. The
+# of the sources it was taken on: the launches, which choose tiles and rings, and what they include,
+# the kernel among it; after a change it is null until re-captured. The
 # counters were taken on 1, 2 and 4 of the workload's 8 sequences (captures of a few GB); each
 # launch's traffic is affine in the sequences (within 1.0%) and is extrapolated to 8.
+CSRC = os.path.join(ROOT, "paper_2604_01622_gb300", "csrc")
 TILE_POLICY = {"auto": 0, "256": 1, "512": 2}   # EC_TILES_AUTO / EC_TILES_256 / EC_TILES_512
 TRAFFIC = {"fc0a0c620a5e": 2895636111}
 
@@ -53,8 +56,19 @@ def _peaks():
     return 6800.0, 1900.0, 1700.0, "fallback"
 
 
-def _src_hash(path):
-    return hashlib.sha1(open(path, "rb").read()).hexdigest()[:12]
+def _src_hash(name="gemm_tc.cu", csrc=CSRC):
+    """Of a source in csrc and of every file there that it includes, directly or through another."""
+    files, todo = [], [name]
+    while todo:
+        f = todo.pop()
+        if f in files or not os.path.exists(os.path.join(csrc, f)):
+            continue
+        files.append(f)
+        todo += re.findall(r'^\s*#include "([^"/]+)"', open(os.path.join(csrc, f)).read(), re.M)
+    h = hashlib.sha1()
+    for f in sorted(files):
+        h.update(f.encode() + b"\0" + open(os.path.join(csrc, f), "rb").read() + b"\0")
+    return h.hexdigest()[:12]
 
 
 def _cores():
@@ -714,9 +728,8 @@ def run_ours(args):
     res = measure(w, args, device, ws, local, headline=True)
     hbm, bf16_burst, bf16_sust, peak_src = _peaks()
     gemm_tflops = res["gemm_tflops"]
-    src = os.path.join(ROOT, "paper_2604_01622_gb300", "csrc", "gemm_tc_kernel.cuh")
     # captured on the default workload's expert-choice step
-    tr = (TRAFFIC.get(_src_hash(src)) if w is I.WORKLOADS["ec_d2048_e64"] and not tc
+    tr = (TRAFFIC.get(_src_hash()) if w is I.WORKLOADS["ec_d2048_e64"] and not tc
           and args.tiles == "auto" else None)
     roofline = {
         "kernel": "tc_gemm_kernel (tcgen05 grouped expert GEMMs: gate/up, down, dU, dH, dW)",
