@@ -364,8 +364,9 @@ ec_status ec_tc_balance(ec_ctx* ctx, float coef, const uint8_t* mask, float* los
  * when they add, up to 1.7e-4 of a sum of one sign whatever its length, a twentieth of what rounding to bf16
  * may take. fp32 products of more than 16 rows (small weights: 48), and the backward call's, split each
  * operand into three bf16 parts (what is left out is 2^-22 of a product); against 64 bits the sum errs by
- * 3e-7 in the root mean square whatever its length. An infinite operand, or one above the largest bf16
- * (3.39e38), gives NaN there where IEEE products may give infinities.
+ * 3e-7 in the root mean square whatever its length. Operands below 2e-34 lose bits there, as the parts are
+ * multiples of 2^-133 (1e-38: 1e-3). An infinite operand, or one above the largest bf16 (3.39e38), gives NaN
+ * there where IEEE products may give infinities.
  * ec_linear_backward: from dY, with dP = drop(dY) act'(P) (rounded to the dtype before the products):
  *   dX = dP W^T [rows][K], dW = X^T dP [K][N], db = column sums of dP [N]; each NULL to skip, in the
  *   context's dtype, overwritten, no overlap with the inputs or one another. P is what the forward

@@ -130,7 +130,8 @@ linear_rows_kernel(const T* __restrict__ X, const T* __restrict__ W, LinearEpi<T
 
 // ------------------------------------------------------------------ fp32 as three bf16 planes
 // x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1); both differences are exact in fp32. Where x is
-// not finite (or rounds to infinity) x1 = x2 = 0.
+// not finite (or rounds to infinity) x1 = x2 = 0. The smallest bf16 is 2^-133: below 2^-109 x2 has fewer
+// bits, below 2^-117 x1 too.
 __device__ __forceinline__ void split3(float x, float* p) {
   p[0] = __bfloat162float(__float2bfloat16_rn(x));
   const float r = fabsf(p[0]) <= 3.4e38f ? x - p[0] : 0.f;
