@@ -45,7 +45,7 @@ UNIT = "tokens/s"
 # launch's traffic is affine in the sequences (within 1.0%) and is extrapolated to 8.
 CSRC = os.path.join(ROOT, "paper_2604_01622_gb300", "csrc")
 TILE_POLICY = {"auto": 0, "256": 1, "512": 2}   # EC_TILES_AUTO / EC_TILES_256 / EC_TILES_512
-TRAFFIC = {"fc0a0c620a5e": 2895636111}
+TRAFFIC = {"0a90c2ea5e62": 2888652998}
 
 
 def _peaks():
