@@ -12,8 +12,8 @@
 // integers and draw tickets, which say who joins and not what is added to what.
 //
 // The loss is bounded by latency: a launch, a chunk's reads and the joins' after them. 65536 tokens of 128
-// experts in 33 sequences, with a mask: 11.0 us for 36 MB (3.3 TB/s), 32768 x 64: 8.1 us, 256 x 8: 6.1 us.
-// The gradient is bounded by memory: 11.2 us for 67 MB (6.0 TB/s, 0.88 of a plain copy), 3.8 and 1.9 us.
+// experts in 33 sequences, with a mask: 11.0 us for 36 MB (3.3 TB/s), 32768 x 64: 8.1 us, 256 x 8: 5.8 us.
+// The gradient is bounded by memory: 11.4 us for 67 MB (5.9 TB/s, 0.87 of a plain copy), 3.9 and 1.9 us.
 #include <algorithm>
 
 #include "common.cuh"
